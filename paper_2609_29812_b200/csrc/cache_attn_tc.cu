@@ -31,7 +31,8 @@ static_assert(2 * kRegsSoftmax + kRegsIssue + kRegsCodes <= 4 * 128, "more regis
 
 struct alignas(16) Factors {   // of a chunk's groups of 16 tokens
   int row[8];               // first row of each in the pools
-  uint32_t spoils;          // groups of blocks without scales that are numbers: their keys are none, and so is what sees them
+  uint32_t spoils;          // bit g: group g is of a block without scales that are numbers: its keys are none, and so is what sees them;
+                            // bit 8 + g: of a block of keys whose scale is zero: so are its keys
   float ks[8], lv[8], iv[8];
   float rv, vref;           // old vref over the new one, the new one: negative where a value of the open block is no number
 };
@@ -119,19 +120,23 @@ __device__ __forceinline__ float max16(const uint32_t* r) {
   for (int i = 0; i < 4; ++i) m[i] = fmaxf(m[i], __uint_as_float(r[12 + i]));
   return fmaxf(max3(m[0], m[1], m[2]), m[3]);
 }
+// Log2 of a probability per unit of a product. Never zero, which would make a number of a hidden column's -inf no number; the
+// smallest normal number beside it is lost in the rounding, or leaves products (below 2^37) as good as zero. (As fmaxf(ks * c2, 2^-126) it
+// cost 3% of a long chunk.)
+__device__ __forceinline__ float logit_unit(float ks, float c2) { return fmaf(ks, c2, 0x1p-126f); }
 // 32 columns (block q of a chunk) whose groups of 16 share their factors where pages are of 32 tokens and more.
 template <bool FINE>
 __device__ __forceinline__ float max_block(const uint32_t (&r)[32], const Factors& f, int q, float c2) {
-  if (FINE) return fmaxf(max16(r) * (f.ks[2 * q] * c2), max16(r + 16) * (f.ks[2 * q + 1] * c2));
-  return max32(r) * (f.ks[2 * q] * c2);
+  if (FINE) return fmaxf(max16(r) * logit_unit(f.ks[2 * q], c2), max16(r + 16) * logit_unit(f.ks[2 * q + 1], c2));
+  return max32(r) * logit_unit(f.ks[2 * q], c2);
 }
 template <bool FINE>
 __device__ __forceinline__ float exp_block(const uint32_t (&r)[32], const Factors& f, int q, float c2, float sub, uint32_t (&p)[16]) {
   if (FINE) {
-    const float a = exp_some<16>(r, f.ks[2 * q] * c2, f.lv[2 * q] - sub, p) * f.iv[2 * q];
-    return a + exp_some<16>(r + 16, f.ks[2 * q + 1] * c2, f.lv[2 * q + 1] - sub, p + 8) * f.iv[2 * q + 1];
+    const float a = exp_some<16>(r, logit_unit(f.ks[2 * q], c2), f.lv[2 * q] - sub, p) * f.iv[2 * q];
+    return a + exp_some<16>(r + 16, logit_unit(f.ks[2 * q + 1], c2), f.lv[2 * q + 1] - sub, p + 8) * f.iv[2 * q + 1];
   }
-  return exp_some<32>(r, f.ks[2 * q] * c2, f.lv[2 * q] - sub, p) * f.iv[2 * q];
+  return exp_some<32>(r, logit_unit(f.ks[2 * q], c2), f.lv[2 * q] - sub, p) * f.iv[2 * q];
 }
 
 // FINE: pages of 16 tokens, factors for every 16 columns.
@@ -219,16 +224,16 @@ __global__ void __launch_bounds__(kThreadsTc, 1) cache_flash_kernel(const __grid
     for_each_plan(true, [&](const Plan& pl) {
       const Segment& g = pl.g;
       const int chunks = pl.chunks;
-      // rows of the tile that are no codes: the open block's, those past the sequence's end, and keys of blocks without scales
+      // rows of the tile that are no codes: the open block's, those past the sequence's end, and keys of blocks without scales or of scale zero
       auto patch = [&](int n, float mul, uint32_t spoils, uint8_t* dst) {
 #pragma unroll 1
         for (int i = 0; i < 64 / kStep; ++i) {
           const int r = row0 + r0 + i * kStep, t = n * 128 + r;
-          const bool spoiled = side == 0 && (spoils >> (r >> 4) & 1u);
-          if (t < pl.full && !spoiled) continue;
+          const uint32_t odd = side == 0 ? spoils >> (r >> 4) & 0x101u : 0u;
+          if (t < pl.full && odd == 0) continue;
           uint4 x, y;
           x = y = make_uint4(0u, 0u, 0u, 0u);
-          if (spoiled) x = y = make_uint4(0x7e007e00u, 0x7e007e00u, 0x7e007e00u, 0x7e007e00u);
+          if (odd & 1u) x = y = make_uint4(0x7e007e00u, 0x7e007e00u, 0x7e007e00u, 0x7e007e00u);
           const int slot = t >= pl.full && t < g.len ? cache_slot(a.c, g.b, a.status) : -1;
           if (slot >= 0) {                                 // a value that is no number is left out here
             const uint4* p = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.c.open[side]) +
@@ -394,7 +399,8 @@ __global__ void __launch_bounds__(kThreadsTc, 1) cache_flash_kernel(const __grid
           Factors& f = ctl.fac[N & 3];
           if (N >= 4 && ok) ok = patient_warp(&ctl.fac_free[N & 3], ((N >> 2) - 1) & 1, abort_flag);
           const bool coded = t < pl.full, spoiled = coded && !(ks1 < INFINITY && vs1 < INFINITY);
-          const uint32_t spoils = __ballot_sync(0xffffffffu, spoiled && lane < 8);
+          const bool zero = coded && ks1 == 0.f;
+          const uint32_t spoils = __ballot_sync(0xffffffffu, spoiled && lane < 8) | __ballot_sync(0xffffffffu, zero && lane < 8) << 8;
           if (lane == 0) f.spoils = spoils;
           if (lane < 8) f.row[lane] = coded ? ((id1 * a.c.n_kv + g.kvh) << a.page_shift) + (t & (a.page - 1)) : 0;
           __syncwarp();
@@ -407,7 +413,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) cache_flash_kernel(const __grid
             odd = open_powers(ctl.top[opens & 1], &mul, &kinv, &mul, &vinv);
             ++opens;
           }
-          const float k1 = coded ? (spoiled ? 1.f : ks1) : t < g.len ? kinv : 1.f, v1 = coded ? (spoiled ? 0.f : vs1) : t < g.len ? vinv : 0.f;
+          const float k1 = coded ? (spoiled || zero ? 1.f : ks1) : t < g.len ? kinv : 1.f, v1 = coded ? (spoiled ? 0.f : vs1) : t < g.len ? vinv : 0.f;
           const float now = fmaxf(vref, __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v1))));
           const float v2 = v1 == 0.f ? now : v1;             // (codes that are all zero: any scale)
           if (lane < 8) {

@@ -1,0 +1,66 @@
+"""Attention over a paged 8-bit cache that holds values at the ends of their range, against the 64-bit form: the kernel of few rows, the
+one of chunks (more than 128 rows of a sequence) and the one of binary32 storage have to agree with the definition and so with each other."""
+import math
+
+import pytest
+
+import cache_reference as ref
+from test_gpu_cache import Cache, env, ints, rows, same_bits  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+DEV = "cuda:0"
+
+KERNELS = [("bf16", 3), ("bf16", 16), ("bf16", 290), ("f32", 16), ("f32", 290)]
+
+
+# ------------------------------------------------------------------------------------------------
+# keys and values that are zeros
+# ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,new", KERNELS)
+@pytest.mark.parametrize("page,code,dim", [(16, "int8", 128), (64, "e4m3", 128), (64, "int8", 64), (16, "e4m3", 64), (128, "int8", 128)])
+def test_blocks_of_zero_keys(env, dtype, new, page, code, dim):
+    """Padding tokens: whole blocks of zero keys before a row, around it and after it."""
+    B, ctx = env
+    c = Cache(B, 3, 700, page=page, code=code, dtype=dtype, n_kv=2, dim=dim)
+    g = torch.Generator().manual_seed(31)
+    lens = [650, 310, new]
+    n = sum(lens)
+    k = rows(g, n, 2, dim, c.dt)
+    for first, end in ((64, 128), (256, 384), (500, 640), (650 + 128, 650 + 256), (650 + 310, 650 + 310 + min(new, 128))):
+        k[first:end, 0] = 0.0
+    k[128:256, 1] = 1e-33                                      # below 2^-100: the same
+    c.append(ctx, lens, k, rows(g, n, 2, dim, c.dt), check=False)
+    c.check_attention(ctx, rows(g, 3 * new, 4, dim, c.dt), [new] * 3, f"{dtype} {new}")
+
+
+@pytest.mark.parametrize("dtype,new", KERNELS)
+@pytest.mark.parametrize("page,dim", [(16, 128), (64, 64)])
+def test_zero_queries_beside_zero_keys(env, dtype, new, page, dim):
+    """Rows of zeros, as queries and as the open block's keys: every logit is zero, a row's output the mean of the values that it sees."""
+    B, ctx = env
+    c = Cache(B, 2, 400, page=page, dtype=dtype, n_kv=1, dim=dim)
+    g = torch.Generator().manual_seed(32)
+    lens = [page * (300 // page) + 9, page * (256 // page) + page - 1]
+    k = rows(g, sum(lens), 1, dim, c.dt)
+    k[lens[0] - 9:lens[0]] = 0.0
+    k[lens[0] + 100:] = 0.0
+    c.append(ctx, lens, k, rows(g, sum(lens), 1, dim, c.dt), check=False)
+    q = rows(g, 2 * new, 2, dim, c.dt)
+    q[::2, 0] = 0.0
+    q[1::2, 1] = 1e-36
+    c.check_attention(ctx, q, [new] * 2, f"{dtype} {new}")
+
+
+@pytest.mark.parametrize("dtype,new", KERNELS)
+def test_rows_that_see_nothing_beside_zero_keys(env, dtype, new):
+    B, ctx = env
+    c = Cache(B, 2, 400, page=16, dtype=dtype, n_kv=1, dim=64)
+    g = torch.Generator().manual_seed(33)
+    lens = [max(1, new - 5), max(1, new // 2)]
+    k = rows(g, sum(lens), 1, 64, c.dt)
+    k[:lens[0] // 16 * 16] = 0.0
+    c.append(ctx, lens, k, rows(g, sum(lens), 1, 64, c.dt), check=False)
+    o, lse = c.check_attention(ctx, rows(g, 2 * new, 1, 64, c.dt), [new] * 2, f"{dtype} {new}")
+    unseen = new - lens[0]
+    assert not o[:max(0, unseen)].any() and torch.isneginf(lse[:max(0, unseen)]).all()
