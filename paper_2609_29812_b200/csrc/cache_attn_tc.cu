@@ -415,11 +415,12 @@ __global__ void __launch_bounds__(kThreadsTc, 1) cache_flash_kernel(const __grid
           }
           const float k1 = coded ? (spoiled || zero ? 1.f : ks1) : t < g.len ? kinv : 1.f, v1 = coded ? (spoiled ? 0.f : vs1) : t < g.len ? vinv : 0.f;
           const float now = fmaxf(vref, __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v1))));
-          const float v2 = v1 == 0.f ? now : v1;             // (codes that are all zero: any scale)
+          // (codes that are all zero: any scale.) Below 2^-60 the probabilities' sum would be lost with them; as f16 they are zeros from 2^-40 on
+          const float share = v1 == 0.f ? 1.f : fmaxf(v1 / now, 0x1p-60f);
           if (lane < 8) {
             f.ks[lane] = k1;
-            f.lv[lane] = log2f(128.f * (v2 / now));
-            f.iv[lane] = now / v2 * 0x1p-7f;
+            f.lv[lane] = log2f(128.f * share);
+            f.iv[lane] = 0x1p-7f / share;
           }
           if (lane == 0) {
             f.rv = vref / now;

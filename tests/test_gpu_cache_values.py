@@ -64,3 +64,25 @@ def test_rows_that_see_nothing_beside_zero_keys(env, dtype, new):
     o, lse = c.check_attention(ctx, rows(g, 2 * new, 1, 64, c.dt), [new] * 2, f"{dtype} {new}")
     unseen = new - lens[0]
     assert not o[:max(0, unseen)].any() and torch.isneginf(lse[:max(0, unseen)]).all()
+
+
+# ------------------------------------------------------------------------------------------------
+# values far apart
+# ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,new", KERNELS)
+@pytest.mark.parametrize("page,code", [(16, "int8"), (64, "e4m3"), (128, "int8")])
+def test_values_of_very_different_size(env, dtype, new, page, code):
+    """Blocks of values around 1e30, 1, 1e-20 and 0 in every order: log-normalisers do not know values, outputs are those of the formula."""
+    B, ctx = env
+    c = Cache(B, 4, 900, page=page, code=code, dtype=dtype, n_kv=2, dim=64)
+    g = torch.Generator().manual_seed(34)
+    lens = [807, 640, 300 + new, 513]
+    k, v = rows(g, sum(lens), 2, 64, c.dt), rows(g, sum(lens), 2, 64, torch.float32)
+    sizes = [[1e30, 1e-20, 0.0, 1.0, 1e-12, 1e30, 1e-30], [1e-20, 1e30, 1.0, 0.0, 1e-12], [0.0, 1e-30, 1e-12, 1e30, 1.0], [1.0, 1e30, 1e-20, 1e-35, 0.0]]
+    at = 0
+    for n, order in zip(lens, sizes):
+        for j in range(0, n, 128):
+            v[at + j:at + min(j + 128, n), 0] *= order[j // 128 % len(order)]
+        at += n
+    c.append(ctx, lens, k, v.to(c.dt), check=False)
+    c.check_attention(ctx, rows(g, 4 * new, 4, 64, c.dt), [new] * 4, f"{dtype} {new}")
