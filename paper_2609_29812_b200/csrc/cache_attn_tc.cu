@@ -32,7 +32,8 @@ static_assert(2 * kRegsSoftmax + kRegsIssue + kRegsCodes <= 4 * 128, "more regis
 struct alignas(16) Factors {   // of a chunk's groups of 16 tokens
   int row[8];               // first row of each in the pools
   uint32_t spoils;          // bit g: group g is of a block without scales that are numbers: its keys are none, and so is what sees them;
-                            // bit 8 + g: of a block of keys whose scale is zero: so are its keys
+                            // bits 8 + g, 24 + g: of a block whose keys, values have scale zero: so are they, whatever the codes (and the
+                            // values of a block without a scale, which only rows meet that do not see it or are none already)
   float ks[8], lv[8], iv[8];
   float rv, vref;           // old vref over the new one, the new one: negative where a value of the open block is no number
 };
@@ -224,12 +225,12 @@ __global__ void __launch_bounds__(kThreadsTc, 1) cache_flash_kernel(const __grid
     for_each_plan(true, [&](const Plan& pl) {
       const Segment& g = pl.g;
       const int chunks = pl.chunks;
-      // rows of the tile that are no codes: the open block's, those past the sequence's end, and keys of blocks without scales or of scale zero
+      // rows of the tile that are no codes: the open block's, those past the sequence's end, and blocks without scales or of scale zero
       auto patch = [&](int n, float mul, uint32_t spoils, uint8_t* dst) {
 #pragma unroll 1
         for (int i = 0; i < 64 / kStep; ++i) {
           const int r = row0 + r0 + i * kStep, t = n * 128 + r;
-          const uint32_t odd = side == 0 ? spoils >> (r >> 4) & 0x101u : 0u;
+          const uint32_t odd = spoils >> (16 * side + (r >> 4)) & 0x101u;
           if (t < pl.full && odd == 0) continue;
           uint4 x, y;
           x = y = make_uint4(0u, 0u, 0u, 0u);
@@ -399,8 +400,9 @@ __global__ void __launch_bounds__(kThreadsTc, 1) cache_flash_kernel(const __grid
           Factors& f = ctl.fac[N & 3];
           if (N >= 4 && ok) ok = patient_warp(&ctl.fac_free[N & 3], ((N >> 2) - 1) & 1, abort_flag);
           const bool coded = t < pl.full, spoiled = coded && !(ks1 < INFINITY && vs1 < INFINITY);
-          const bool zero = coded && ks1 == 0.f;
-          const uint32_t spoils = __ballot_sync(0xffffffffu, spoiled && lane < 8) | __ballot_sync(0xffffffffu, zero && lane < 8) << 8;
+          const bool zero = coded && ks1 == 0.f, nought = spoiled || (coded && vs1 == 0.f);
+          const uint32_t spoils = __ballot_sync(0xffffffffu, spoiled && lane < 8) | __ballot_sync(0xffffffffu, zero && lane < 8) << 8 |
+                                  __ballot_sync(0xffffffffu, nought && lane < 8) << 24;
           if (lane == 0) f.spoils = spoils;
           if (lane < 8) f.row[lane] = coded ? ((id1 * a.c.n_kv + g.kvh) << a.page_shift) + (t & (a.page - 1)) : 0;
           __syncwarp();
@@ -415,7 +417,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) cache_flash_kernel(const __grid
           }
           const float k1 = coded ? (spoiled || zero ? 1.f : ks1) : t < g.len ? kinv : 1.f, v1 = coded ? (spoiled ? 0.f : vs1) : t < g.len ? vinv : 0.f;
           const float now = fmaxf(vref, __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v1))));
-          // (codes that are all zero: any scale.) Below 2^-60 the probabilities' sum would be lost with them; as f16 they are zeros from 2^-40 on
+          // (values that are all zero: any scale.) Below 2^-60 the probabilities' sum would be lost with them; as f16 they are zeros from 2^-40 on
           const float share = v1 == 0.f ? 1.f : fmaxf(v1 / now, 0x1p-60f);
           if (lane < 8) {
             f.ks[lane] = k1;

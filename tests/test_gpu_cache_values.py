@@ -86,3 +86,23 @@ def test_values_of_very_different_size(env, dtype, new, page, code):
         at += n
     c.append(ctx, lens, k, v.to(c.dt), check=False)
     c.check_attention(ctx, rows(g, 4 * new, 4, 64, c.dt), [new] * 4, f"{dtype} {new}")
+
+
+# ------------------------------------------------------------------------------------------------
+# scales that another program wrote
+# ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,new", KERNELS)
+@pytest.mark.parametrize("page,code", [(16, "e4m3"), (64, "int8")])
+def test_scale_zero_beside_codes_that_are_not(env, dtype, new, page, code):
+    """A value is code * scale, whoever wrote the two: keys and values of a block of scale zero are zeros whatever its codes."""
+    B, ctx = env
+    c = Cache(B, 2, 700, page=page, code=code, dtype=dtype, n_kv=1, dim=128)
+    g = torch.Generator().manual_seed(35)
+    lens = [600, 290 + page]
+    c.append(ctx, lens, rows(g, sum(lens), 1, 128, c.dt), rows(g, sum(lens), 1, 128, c.dt), check=False)
+    for b in range(2):
+        for side, step in ((0, 3), (1, 2)):
+            for j in range(1, lens[b] // page, step):
+                c.scale[side][int(c.table_host[b, j])] = 0.0
+                c.rows[side][b][j * page:(j + 1) * page] = 0.0
+    c.check_attention(ctx, rows(g, 2 * new, 2, 128, c.dt), [new] * 2, f"{dtype} {new}")
