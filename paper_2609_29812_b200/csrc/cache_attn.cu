@@ -19,7 +19,8 @@ constexpr int kUnit = 64;          // tokens of a unit
 constexpr int kWarps = 4;
 constexpr int kMostStages = 6;     // tiles of a warp's ring
 
-// The pages of a warp's tiles, 32 at a time: lane i has page `base + i` of the sequence and its scales.
+// The pages of a warp's tiles, 32 at a time: lane i has page `base + i` of the sequence and its scales. A row is none if it sees a block
+// without a scale, whatever its probabilities there: that goes by the logits, since a value's factor is lost where a probability is zero.
 struct PageWindow {
   int base, id;
   float ks, vs;
@@ -31,6 +32,7 @@ struct PageWindow {
       id = max(0, cache_page(a.c, g.b, first + lane, a.status));
       ks = __ldg(a.c.scale[0] + (int64_t)id * a.c.n_kv + g.kvh);
       vs = __ldg(a.c.scale[1] + (int64_t)id * a.c.n_kv + g.kvh);
+      if (!(ks < INFINITY && vs < INFINITY)) ks = __int_as_float(0x7fc00000);   // either is none: so are the logits of the rows that see the block
     }
   }
 };

@@ -106,3 +106,37 @@ def test_scale_zero_beside_codes_that_are_not(env, dtype, new, page, code):
                 c.scale[side][int(c.table_host[b, j])] = 0.0
                 c.rows[side][b][j * page:(j + 1) * page] = 0.0
     c.check_attention(ctx, rows(g, 2 * new, 2, 128, c.dt), [new] * 2, f"{dtype} {new}")
+
+
+# ------------------------------------------------------------------------------------------------
+# blocks with infinities and NaN
+# ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,new", KERNELS)
+@pytest.mark.parametrize("page,code", [(16, "int8"), (64, "e4m3")])
+@pytest.mark.parametrize("side", [0, 1])
+def test_every_row_that_sees_a_block_without_a_scale_is_none(env, dtype, new, page, code, side):
+    """Output and log-normaliser of rows that see a token of the block, also where its tokens' probabilities are zeros beside a dominant
+    key; rows before the block are as without it."""
+    B, ctx = env
+    g = torch.Generator().manual_seed(36)
+    n_seqs, dim = 3, 128
+    lens = [page * (700 // page), page * (420 // page) + 3, page * (330 // page)]
+    c = Cache(B, n_seqs, 720, page=page, code=code, dtype=dtype, n_kv=1, dim=dim)
+    k, v = rows(g, sum(lens), 1, dim, torch.float32, 0.1), rows(g, sum(lens), 1, dim, c.dt)
+    first = []                                                 # tokens before the bad block
+    at = 0
+    for b, (n, dominant, bad) in enumerate(zip(lens, (650, 7, 9), (100, lens[1] - 10, lens[2] - 1))):
+        k[at + dominant] = 4.0                                 # logits 180 above the others: 2^-126 and less is left of those
+        (k if side == 0 else v)[at + bad, 0, 5] = math.inf if b else math.nan
+        first.append(bad // page * page)
+        at += n
+    c.append(ctx, lens, k.to(c.dt), v, check=False)
+    q = (rows(g, n_seqs * new, 2, dim, torch.float32, 0.1) + 4.0).to(c.dt)
+    o, lse = c.attend(ctx, q, [new] * n_seqs)
+    for b in range(n_seqs):
+        s = slice(b * new, (b + 1) * new)
+        blind = max(0, min(new, first[b] - (lens[b] - new)))   # rows that see no token of the block
+        assert torch.isnan(o[s][blind:]).all() and torch.isnan(lse[s][blind:]).all(), b
+        if blind:
+            want = ref.attention(q[s][:blind].double(), c.held(0, b)[:lens[b] - new + blind], c.held(1, b)[:lens[b] - new + blind], 2, dim ** -0.5)
+            ref.assert_attention(o[s][:blind], lse[s][:blind], want, dim, dtype == "bf16", f"sequence {b}")
