@@ -346,6 +346,38 @@ class LayerState:
         return o_out, csn
 
 
+# The library takes addresses. What these objects hand it is looked at here: a tensor of another type, shape or place would be read, or
+# written, past its end.
+def _refuse(call: str, why: str):
+    raise B.FlashLoopError(f"{call} ({why})", B.FL_ERR_INVALID_ARG)
+
+
+def _row_stride(call: str, name: str, x, like, n: int = 0, heads: Optional[int] = None, dim: Optional[int] = None) -> int:
+    """Elements from one row of x [n or more, heads, dim] to the next; its type is one of `like`'s (types, device). A row's heads stand side
+    by side, the rows any distance apart that keeps them so."""
+    types, device = like
+    if x.dim() != 3 or x.shape[0] < n or x.shape[1] != (heads or x.shape[1]) or x.shape[2] != (dim or x.shape[2]):
+        _refuse(call, f"{name} is {list(x.shape)}, not [{n}, {heads or 'heads'}, {dim or 'head_dim'}]")
+    if x.dtype not in types or x.device != device:
+        _refuse(call, f"{name} is {x.dtype} on {x.device}, not {' or '.join(map(str, types))} on {device}")
+    row = x.shape[1] * x.shape[2]
+    if x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]):
+        _refuse(call, f"the heads of a row of {name} do not follow one another")
+    if x.shape[0] <= 1:
+        return row
+    if x.stride(0) < row:
+        _refuse(call, f"the rows of {name} overlap")
+    return x.stride(0)
+
+
+def _indices(call: str, name: str, x, n: int, device):
+    if x is not None and (x.dim() != 1 or x.numel() < n or x.dtype != torch.int32 or x.device != device or not x.is_contiguous()):
+        _refuse(call, f"{name} is {x.dtype} {list(x.shape)} on {x.device}, not {n} contiguous int32 on {device}")
+
+
+_STORAGE = {torch.bfloat16: B.FL_BF16, torch.float32: B.FL_F32}
+
+
 class RotaryTable:
     """Cosines and sines of positions 0 .. n_pos - 1, and the two descriptors that a rotation needs."""
 
@@ -357,17 +389,15 @@ class RotaryTable:
 
     def rotate(self, x, pos, inverse: bool = False, out=None, pos0: int = 0):
         """x: [n, heads, head_dim], rows any distance apart (a part of a stacked projection); pos: int32 [n], or None for pos0, pos0 + 1, ..."""
+        like = (tuple(_STORAGE), self.table.device)
+        stride = _row_stride("RotaryTable.rotate", "x", x, like)
         n, heads, dim = x.shape
-        out = torch.empty(n, heads, dim, dtype=x.dtype, device=x.device) if out is None else out
-        B.fl_rotate_rows(self.ctx, x, _row_stride(x), pos, n, heads, dim, B.FL_BF16 if x.dtype == torch.bfloat16 else B.FL_F32, self.rope,
-                         inverse, out, _row_stride(out), pos0=pos0)
+        _indices("RotaryTable.rotate", "pos", pos, n, self.table.device)
+        if out is None:
+            out = torch.empty(n, heads, dim, dtype=x.dtype, device=x.device)
+        out_stride = _row_stride("RotaryTable.rotate", "out", out, ((x.dtype,), x.device), n, heads, dim)
+        B.fl_rotate_rows(self.ctx, x, stride, pos, n, heads, dim, _STORAGE[x.dtype], self.rope, inverse, out, out_stride, pos0=pos0)
         return out
-
-
-def _row_stride(x) -> int:
-    """Elements from one row of [n, heads, head_dim] to the next; a row's heads stand side by side."""
-    assert x.stride(2) == 1 and x.stride(1) == x.shape[2], "a row's heads must follow one another"
-    return max(x.stride(0), x.shape[1] * x.shape[2]) if x.shape[0] > 1 else max(x.shape[1] * x.shape[2], x.stride(0))
 
 
 class PagedCache:
@@ -376,8 +406,10 @@ class PagedCache:
 
     def __init__(self, ctx, n_seqs: int, n_kv_heads: int, head_dim: int, max_tokens: int, n_pages: Optional[int] = None, page: int = 64,
                  dtype=torch.bfloat16, code=B.FL_INT8, device="cuda:0"):
+        if dtype not in _STORAGE or code not in (B.FL_INT8, B.FL_E4M3):
+            _refuse("PagedCache", f"storage {dtype}, code {code}")
         self.ctx, self.dev = ctx, _device(device)
-        self.n_seqs, self.page, self.dtype = n_seqs, page, dtype
+        self.n_seqs, self.page, self.dtype, self.n_kv_heads, self.head_dim = n_seqs, page, dtype, n_kv_heads, head_dim
         self.max_pages = max(1, -(-max_tokens // page))
         n_pages = n_seqs * self.max_pages if n_pages is None else n_pages
         ct = torch.int8 if code == B.FL_INT8 else torch.float8_e4m3fn
@@ -392,14 +424,20 @@ class PagedCache:
         self.len_dev = torch.zeros(n_seqs, dtype=torch.int32, device=self.dev)
         self.status = status_word(self.dev)
         self.handle = B.make_paged_kv(self.k_codes, self.v_codes, self.k_scale, self.v_scale, self.k_open, self.v_open, self.page_table,
-                                      page=page, dtype=B.FL_BF16 if dtype == torch.bfloat16 else B.FL_F32, code=code)
+                                      page=page, dtype=_STORAGE[dtype], code=code)
         self._workspace = None
 
     def _ints(self, v):
         return torch.tensor(v, dtype=torch.int32, device=self.dev)
 
+    def _counts(self, call: str, new: List[int]) -> int:
+        if len(new) != self.n_seqs or any(n < 0 for n in new):
+            _refuse(call, f"new is {list(new)}, not a number of tokens for each of {self.n_seqs} sequences")
+        return sum(new)
+
     def reserve(self, new: List[int]):
         """Pages for the blocks that `new` more tokens per sequence complete."""
+        self._counts("PagedCache.reserve", new)
         for b, n in enumerate(new):
             while len(self.pages[b]) < (self.lens[b] + n) // self.page:
                 if not self.free or len(self.pages[b]) >= self.max_pages:
@@ -416,10 +454,16 @@ class PagedCache:
 
     def append(self, k, v, new: List[int], rotary: Optional[RotaryTable] = None, pos=None):
         """k, v: [sum(new), n_kv_heads, head_dim], new[b] rows for sequence b; keys are rotated on the way where `rotary` is given."""
+        call, like = "PagedCache.append", ((self.dtype,), self.dev)
+        n = self._counts(call, new)
+        strides = [_row_stride(call, name, x, like, n, self.n_kv_heads, self.head_dim) for name, x in (("k", k), ("v", v))]
+        _indices(call, "pos", pos, n, self.dev)
+        if rotary is not None and rotary.table.device != self.dev:
+            _refuse(call, f"the rotation's table is on {rotary.table.device}, not on {self.dev}")
         self.reserve(new)
         starts = self._ints(list(itertools.accumulate(new, initial=0)))
         after = torch.empty_like(self.len_dev)
-        B.fl_cache_append(self.ctx, self.handle, rotary.rope if rotary is not None else None, k, _row_stride(k), v, _row_stride(v), starts, sum(new),
+        B.fl_cache_append(self.ctx, self.handle, rotary.rope if rotary is not None else None, k, strides[0], v, strides[1], starts, n,
                           self.len_dev, after, pos=pos, status=self.status)
         self.len_dev = after
         self.lens = [a + n for a, n in zip(self.lens, new)]
@@ -427,21 +471,30 @@ class PagedCache:
 
     def attend(self, q, new: List[int], sm_scale: float, starts=None):
         """Attention of the last new[b] tokens of each sequence (their rows are in the cache): outputs [n, heads, head_dim] and
-        log-normalisers [n, heads], which are what fl_decode_attention takes as o_prev and lse_prev."""
+        log-normalisers [n, heads], which are what fl_decode_attention takes as o_prev and lse_prev.  Sequence b has rows starts[b] ..
+        starts[b + 1] - 1 of q (int32 on the device, as append returns them; None: one sequence after the other)."""
+        call, total = "PagedCache.attend", self._counts("PagedCache.attend", new)
+        stride = _row_stride(call, "q", q, ((self.dtype,), self.dev), total, None, self.head_dim)
         n, heads, dim = q.shape
-        starts = self._ints(list(itertools.accumulate(new, initial=0))) if starts is None else starts
+        if starts is None:
+            if n != total:
+                _refuse(call, f"q has {n} rows, not {total}")
+            starts = self._ints(list(itertools.accumulate(new, initial=0)))
+        _indices(call, "starts", starts, self.n_seqs + 1, self.dev)
         max_q = max(max(new), 1)
         need = B.fl_cache_attention_workspace_bytes(self.ctx, self.handle, heads, n, max_q)
         if self._workspace is None or self._workspace.numel() < need:
             self._workspace = torch.zeros(need, dtype=torch.uint8, device=self.dev)
         o = torch.empty(n, heads, dim, dtype=self.dtype, device=self.dev)
         lse = torch.empty(n, heads, dtype=torch.float32, device=self.dev)
-        B.fl_cache_attention(self.ctx, self.handle, q, _row_stride(q), heads, starts, n, max_q, self.len_dev, sm_scale, o, lse, self._workspace,
+        B.fl_cache_attention(self.ctx, self.handle, q, stride, heads, starts, n, max_q, self.len_dev, sm_scale, o, lse, self._workspace,
                              self._workspace.numel(), status=self.status)
         return o, lse
 
     def read(self, b: int, first: int = 0, n: Optional[int] = None):
         """Rows first .. first + n - 1 of a sequence as the cache holds them, in the storage type: a base for the sparse loops."""
+        if not 0 <= b < self.n_seqs or first < 0 or (n is not None and n < 0) or (n is None and first > self.lens[b]):
+            _refuse("PagedCache.read", f"rows {first} on, {n} of them, of sequence {b}")
         n = self.lens[b] - first if n is None else n
         k = torch.empty(n, *self.k_open.shape[1:2], self.k_open.shape[3], dtype=self.dtype, device=self.dev)
         v = torch.empty_like(k)
