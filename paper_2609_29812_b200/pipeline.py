@@ -402,7 +402,8 @@ class RotaryTable:
 
 class PagedCache:
     """A paged 8-bit K/V cache of one layer and the calls on it: pages are handed out on the host as sequences grow, everything else stays
-    on the device.  `code`: B.FL_INT8 or B.FL_E4M3."""
+    on the device.  `code`: B.FL_INT8 or B.FL_E4M3.  On more than one stream calls are ordered by the program, as with any tensors: append
+    and release write what attend and read look at.  Those two may run beside one another; each stream has a workspace of its own."""
 
     def __init__(self, ctx, n_seqs: int, n_kv_heads: int, head_dim: int, max_tokens: int, n_pages: Optional[int] = None, page: int = 64,
                  dtype=torch.bfloat16, code=B.FL_INT8, device="cuda:0"):
@@ -425,7 +426,26 @@ class PagedCache:
         self.status = status_word(self.dev)
         self.handle = B.make_paged_kv(self.k_codes, self.v_codes, self.k_scale, self.v_scale, self.k_open, self.v_open, self.page_table,
                                       page=page, dtype=_STORAGE[dtype], code=code)
-        self._workspace = None
+        self._workspaces = {}                                      # by stream: calls that may overlap must not share one
+        self._len_stream = self._stream()                          # where len_dev was allocated
+
+    def _stream(self):
+        return B._stream_of(self.dev.index)
+
+    def _lens_read_here(self):
+        """The next append drops len_dev: on another stream than its own the allocator has to hear of this use."""
+        if self._stream() != self._len_stream:
+            self.len_dev.record_stream(torch.cuda.current_stream(self.dev))
+
+    def _workspace(self, need: int):
+        """Cleared once, on the stream that uses it; a call leaves it cleared.  Under graph capture a clear is recorded and not executed:
+        there a workspace is an allocation of its own, which every replay clears."""
+        if torch.cuda.is_current_stream_capturing():
+            return torch.zeros(need, dtype=torch.uint8, device=self.dev)
+        ws = self._workspaces.get(self._stream())
+        if ws is None or ws.numel() < need:
+            ws = self._workspaces[self._stream()] = torch.zeros(need, dtype=torch.uint8, device=self.dev)
+        return ws
 
     def _ints(self, v):
         return torch.tensor(v, dtype=torch.int32, device=self.dev)
@@ -465,7 +485,8 @@ class PagedCache:
         after = torch.empty_like(self.len_dev)
         B.fl_cache_append(self.ctx, self.handle, rotary.rope if rotary is not None else None, k, strides[0], v, strides[1], starts, n,
                           self.len_dev, after, pos=pos, status=self.status)
-        self.len_dev = after
+        self._lens_read_here()
+        self.len_dev, self._len_stream = after, self._stream()
         self.lens = [a + n for a, n in zip(self.lens, new)]
         return starts
 
@@ -483,12 +504,12 @@ class PagedCache:
         _indices(call, "starts", starts, self.n_seqs + 1, self.dev)
         max_q = max(max(new), 1)
         need = B.fl_cache_attention_workspace_bytes(self.ctx, self.handle, heads, n, max_q)
-        if self._workspace is None or self._workspace.numel() < need:
-            self._workspace = torch.zeros(need, dtype=torch.uint8, device=self.dev)
+        ws = self._workspace(need)
         o = torch.empty(n, heads, dim, dtype=self.dtype, device=self.dev)
         lse = torch.empty(n, heads, dtype=torch.float32, device=self.dev)
-        B.fl_cache_attention(self.ctx, self.handle, q, stride, heads, starts, n, max_q, self.len_dev, sm_scale, o, lse, self._workspace,
-                             self._workspace.numel(), status=self.status)
+        B.fl_cache_attention(self.ctx, self.handle, q, stride, heads, starts, n, max_q, self.len_dev, sm_scale, o, lse, ws, ws.numel(),
+                             status=self.status)
+        self._lens_read_here()
         return o, lse
 
     def read(self, b: int, first: int = 0, n: Optional[int] = None):
@@ -501,6 +522,7 @@ class PagedCache:
         starts = self._ints([0] * (b + 1) + [n] * (self.n_seqs - b))
         firsts = self._ints([first if i == b else 0 for i in range(self.n_seqs)])
         B.fl_cache_read(self.ctx, self.handle, starts, firsts, n, self.len_dev, k, v, status=self.status)
+        self._lens_read_here()
         return k, v
 
     def check_status(self):

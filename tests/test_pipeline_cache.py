@@ -19,7 +19,8 @@ def host(monkeypatch):
     for name in ("fl_rope_table", "fl_rotate_rows", "fl_cache_append", "fl_cache_read", "fl_cache_attention"):
         monkeypatch.setattr(B, name, record(name))
     monkeypatch.setattr(B, "fl_cache_attention_workspace_bytes", lambda *a: 256)
-    monkeypatch.setattr(B, "_stream_of", lambda index: None)
+    monkeypatch.setattr(B, "_stream_of", lambda index: P.__dict__.get("test_stream"))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     monkeypatch.setattr(P, "status_word", lambda dev: torch.zeros(1, dtype=torch.int32))
     return P, B, calls
 
@@ -109,3 +110,32 @@ def test_attend_and_read_take_what_they_read(host):
     assert calls[-1][1][6] == 9 and o.shape[0] == 9
     k, v = c.read(1, 0, 4)
     assert calls[-1][0] == "fl_cache_read" and k.shape == v.shape == (4, 2, 64)
+
+
+def test_calls_on_different_streams_share_no_workspace(host, monkeypatch):
+    P, B, calls = host
+    need, used = [256], []
+    monkeypatch.setattr(B, "fl_cache_attention_workspace_bytes", lambda *a: need[0])
+    c = P.PagedCache(None, 1, 1, 64, 100, page=16, device="cpu")
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, s: used.append((self.data_ptr(), s)))
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda dev=None: P.test_stream)
+
+    def workspace(stream):
+        monkeypatch.setattr(P, "test_stream", stream, raising=False)
+        c.attend(rows(1, 1), [1], 0.125)
+        assert calls[-1][0] == "fl_cache_attention" and int(calls[-1][1][13]) == calls[-1][1][12].numel()
+        return calls[-1][1][12]
+
+    first, second = workspace(None), workspace(7)
+    assert first.data_ptr() != second.data_ptr() and workspace(None) is first and workspace(7) is second
+    need[0] = 512
+    grown = workspace(7)
+    assert grown.numel() == 512 and workspace(None).numel() == 512 and workspace(None).data_ptr() != grown.data_ptr()
+    # lengths that another stream has read are told to the allocator before the object lets go of them
+    assert used and all(u == (c.len_dev.data_ptr(), 7) for u in used)
+    # a captured call's workspace is the graph's
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    own = workspace(7)
+    assert own is not grown and workspace(7) is not own
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    assert workspace(7) is grown
