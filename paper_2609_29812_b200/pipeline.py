@@ -456,12 +456,16 @@ class PagedCache:
         return sum(new)
 
     def reserve(self, new: List[int]):
-        """Pages for the blocks that `new` more tokens per sequence complete."""
+        """Pages for the blocks that `new` more tokens per sequence complete: all of them, or RuntimeError and none."""
         self._counts("PagedCache.reserve", new)
+        free = len(self.free)
+        for b, n in enumerate(new):
+            blocks = (self.lens[b] + n) // self.page
+            free -= max(0, blocks - len(self.pages[b]))
+            if free < 0 or blocks > self.max_pages:
+                raise RuntimeError(f"no page for sequence {b}")
         for b, n in enumerate(new):
             while len(self.pages[b]) < (self.lens[b] + n) // self.page:
-                if not self.free or len(self.pages[b]) >= self.max_pages:
-                    raise RuntimeError(f"no page for sequence {b}")
                 p = self.free.pop()
                 self.page_table[b, len(self.pages[b])] = p
                 self.pages[b].append(p)

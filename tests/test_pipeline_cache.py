@@ -139,3 +139,16 @@ def test_calls_on_different_streams_share_no_workspace(host, monkeypatch):
     assert own is not grown and workspace(7) is not own
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     assert workspace(7) is grown
+
+
+def test_a_reservation_that_cannot_be_met_takes_no_page(host):
+    P, B, calls = host
+    c = P.PagedCache(None, 3, 1, 64, 64, n_pages=5, page=16, device="cpu")
+    for new in ([32, 0, 65], [33, 32, 32], [0, 80, 0]):                       # more pages than are free, or than a sequence's table holds
+        with pytest.raises(RuntimeError):
+            c.append(rows(sum(new), 1), rows(sum(new), 1), new)
+        assert len(c.free) == 5 and c.pages == [[], [], []] and c.lens == [0, 0, 0]
+    c.append(rows(80, 1), rows(80, 1), [33, 31, 16])
+    assert [len(p) for p in c.pages] == [2, 1, 1] and len(c.free) == 1
+    c.append(rows(1, 1), rows(1, 1), [0, 1, 0])
+    assert not c.free and c.page_table[1, :2].tolist() == c.pages[1]
