@@ -384,11 +384,13 @@ class RotaryTable:
     def __init__(self, ctx, n_pos: int, rot_dim: int, layout=B.FL_ROPE_HALF, kind=B.FL_ROPE_PLAIN, device="cuda:0", **spec):
         self.ctx, self.n_pos = ctx, n_pos
         self.table = torch.empty(n_pos, rot_dim // 2, 2, dtype=torch.float32, device=_device(device))
+        self.status = status_word(self.table.device)
         B.fl_rope_table(ctx, B.make_rope_spec(kind, rot_dim, **spec), self.table, n_pos)
         self.rope = B.make_rope(self.table, n_pos, rot_dim, layout)
 
     def rotate(self, x, pos, inverse: bool = False, out=None, pos0: int = 0):
-        """x: [n, heads, head_dim], rows any distance apart (a part of a stacked projection); pos: int32 [n], or None for pos0, pos0 + 1, ..."""
+        """x: [n, heads, head_dim], rows any distance apart (a part of a stacked projection); pos: int32 [n], or None for pos0, pos0 + 1, ...
+        Positions that the table does not hold are reported by check_status()."""
         like = (tuple(_STORAGE), self.table.device)
         stride = _row_stride("RotaryTable.rotate", "x", x, like)
         n, heads, dim = x.shape
@@ -396,8 +398,15 @@ class RotaryTable:
         if out is None:
             out = torch.empty(n, heads, dim, dtype=x.dtype, device=x.device)
         out_stride = _row_stride("RotaryTable.rotate", "out", out, ((x.dtype,), x.device), n, heads, dim)
-        B.fl_rotate_rows(self.ctx, x, stride, pos, n, heads, dim, _STORAGE[x.dtype], self.rope, inverse, out, out_stride, pos0=pos0)
+        B.fl_rotate_rows(self.ctx, x, stride, pos, n, heads, dim, _STORAGE[x.dtype], self.rope, inverse, out, out_stride, pos0=pos0,
+                         status=self.status)
         return out
+
+    def check_status(self):
+        """Synchronises and raises if a position was outside the table."""
+        code = int(self.status.item())
+        if code != 0:
+            raise B.FlashLoopError("device status", code)
 
 
 class PagedCache:

@@ -28,3 +28,16 @@ def test_two_streams_attend_beside_each_other():
             for o, lse in got[i]:
                 assert torch.equal(o, want[i][0]) and torch.equal(lse, want[i][1])
         c.check_status()
+
+
+def test_positions_outside_a_table_are_reported():
+    from paper_2609_29812_b200 import binding as B, pipeline as P
+    with B.Context(0) as ctx:
+        t = P.RotaryTable(ctx, 10, 64)
+        x = torch.randn(3, 1, 64, device="cuda")
+        t.rotate(x, torch.tensor([0, 9, 5], dtype=torch.int32, device="cuda"))
+        t.check_status()
+        t.rotate(x, torch.tensor([0, 10, 5], dtype=torch.int32, device="cuda"))
+        with pytest.raises(B.FlashLoopError) as e:
+            t.check_status()
+        assert e.value.status == B.FL_ERR_INVALID_ARG

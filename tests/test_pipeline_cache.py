@@ -152,3 +152,15 @@ def test_a_reservation_that_cannot_be_met_takes_no_page(host):
     assert [len(p) for p in c.pages] == [2, 1, 1] and len(c.free) == 1
     c.append(rows(1, 1), rows(1, 1), [0, 1, 0])
     assert not c.free and c.page_table[1, :2].tolist() == c.pages[1]
+
+
+def test_a_rotation_hears_of_positions_outside_its_table(host):
+    P, B, calls = host
+    t = P.RotaryTable(None, 100, 64, device="cpu")
+    t.rotate(rows(1), torch.tensor([100], dtype=torch.int32))
+    assert calls[-1][0] == "fl_rotate_rows" and calls[-1][2]["status"] is t.status
+    t.check_status()
+    t.status.fill_(B.FL_ERR_INVALID_ARG)                                       # as the kernel does
+    with pytest.raises(B.FlashLoopError) as e:
+        t.check_status()
+    assert e.value.status == B.FL_ERR_INVALID_ARG
