@@ -50,7 +50,8 @@ def run(prompt=1100, steps=3, heads=2, dim=128, chunk=400, columns=160, page=64,
         every = torch.arange(prompt, dtype=torch.int32, device=dev)
         sel = P.TokenSelection(every, every.clone(), torch.zeros(prompt, device=dev), prompt)
         delta = lambda x: (x.float() + 0.05 * torch.randn(x.shape, generator=g, device=dev)).to(torch.bfloat16)
-        st.sparse_loop(2, delta(q), delta(k_base), delta(v_base), sel, indexed=True)
+        q2, k2, v2 = delta(q), delta(k_base), delta(v_base)
+        st.sparse_loop(2, q2, k2, v2, sel, indexed=True)
 
         # ---- decode --------------------------------------------------------------------------------------------
         for step in range(steps):
@@ -69,7 +70,7 @@ def run(prompt=1100, steps=3, heads=2, dim=128, chunk=400, columns=160, page=64,
         st.check_status()
         cache.check_status()
         k_all, v_all = cache.read(0)
-        out.update(k=k_all, v=v_all, q=q, o_loop1=torch.cat(out.pop("prompt_o")), lse_loop1=torch.cat(out.pop("prompt_lse")))
+        out.update(k=k_all, v=v_all, q=q, k2=k2, v2=v2, sm_scale=scale, o_loop1=torch.cat(out.pop("prompt_o")), lse_loop1=torch.cat(out.pop("prompt_lse")))
         torch.cuda.synchronize()
     return out
 

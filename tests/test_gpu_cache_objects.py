@@ -41,3 +41,26 @@ def test_positions_outside_a_table_are_reported():
         with pytest.raises(B.FlashLoopError) as e:
             t.check_status()
         assert e.value.status == B.FL_ERR_INVALID_ARG
+
+
+def test_the_example_s_second_loop_starts_from_the_cache():
+    """Loop 2 of the decode steps against the oracle, which takes the prompt's rows as the cache holds them for loop 1, the residuals' codec
+    for loop 2, and loop 1's outputs and log-normalisers as the attention over the cache gave them."""
+    import numpy as np
+
+    from helpers import assert_attn_close, to_np
+    from oracle import flashloop_oracle as fo
+    from test_gpu_cache_path import example
+    prompt, columns, steps = 500, 64, 2                      # (the prompt's last block stays open over both steps)
+    r = example().run(prompt=prompt, steps=steps, chunk=192, columns=columns, page=64)
+    base = [to_np(r[s][:prompt]) for s in ("k", "v")]
+    hat = [fo.residual_update(to_np(r[s + "2"]), b, np.arange(prompt), 4, 128)[0] for s, b in zip("kv", base)]
+    for i, d in enumerate(r["decode"]):
+        q, q2, cols, lse1 = to_np(d["q"]), to_np(d["q2"]), d["cols"].cpu().numpy(), d["lse1"].double().cpu().numpy()
+        heads = q.shape[1]
+        sets = {(0, h): cols[0, h] for h in range(heads)}
+        p_old = {(0, h): np.exp(base[0][cols[0, h], h].astype("f8") @ q[0, h].astype("f8") * r["sm_scale"] - lse1[0, h]) for h in range(heads)}
+        want = fo.decode_sparse_attention(q2, hat[0], hat[1], base[1], to_np(d["o1"]).astype("f8"), sets, p_old, r["sm_scale"], kv_round=fo.round_bf16)
+        assert_attn_close(to_np(d["o2"]), want["O"], f"example, token {i}")
+        np.testing.assert_allclose(to_np(d["lse2"]), want["lse"], rtol=0, atol=5e-3)
+        assert np.linalg.norm(want["O"] - to_np(d["o1"])) > 5 * 1e-2 * np.linalg.norm(want["O"])    # (what loop 2 does is well above the bound)
