@@ -876,7 +876,7 @@ __global__ void __launch_bounds__(kWarps * 32, E::kCtas) cache_attn_kernel(const
 
 template <typename E> constexpr size_t kSmemBytes = 1024 + kMeetingBytes<E> + E::kExtra;   // (tiles stand on 1024-byte boundaries)
 
-constexpr int kMostCtas = 4;       // per SM, of any engine
+constexpr int kMostCtas = 3;       // per SM, of any engine
 
 template <typename E>
 int launch(fl_ctx* ctx, const AttnArgs& a, cudaStream_t st) {
@@ -901,8 +901,8 @@ int check_call(const fl_paged_kv* cache, int32_t n_heads, int32_t n_tokens, int3
   return FL_OK;
 }
 
-// Counters first (of the two kernels), partial results behind them.
-int64_t counter_bytes(const fl_ctx* ctx) { return ((int64_t)ctx->sm_count * (kMostCtas + 1) * 4 + 255) / 256 * 256; }
+// This kernel's counters, its partial results, the chunk kernel's (whose cut problems need no counters).
+int64_t counter_bytes(const fl_ctx* ctx) { return ((int64_t)ctx->sm_count * kMostCtas * 4 + 255) / 256 * 256; }
 int64_t part_bytes(const fl_ctx* ctx, int head_dim) {
   return ((int64_t)ctx->sm_count * kMostCtas * 2 * kFewRows * (head_dim + 2) * 4 + 255) / 256 * 256;
 }
@@ -979,7 +979,6 @@ extern "C" int fl_cache_attention(fl_ctx* ctx, const fl_paged_kv* cache, const v
     rc2 = cache->code == FL_INT8 ? launch_rows<64, FL_INT8>(ctx, a, cache->dtype, rows, st) : launch_rows<64, FL_E4M3>(ctx, a, cache->dtype, rows, st);
   if (rc2 != FL_OK || !chunks) return rc2;
   a.which = kMany;
-  a.counters += ctx->sm_count * kMostCtas;
   a.part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.part) + part_bytes(ctx, cache->head_dim));
   return fl_launch_cache_attn_tc(ctx, a, cache->head_dim, cache->code, st);
 }

@@ -21,7 +21,7 @@ struct alignas(64) AttnArgs {
   const int32_t* kv_len;
   void* o;
   float* lse;
-  int32_t* counters;         // arrivals at split problems, zero between calls
+  int32_t* counters;         // arrivals at split problems (few rows), zero between calls
   float* part;               // partial results: per CTA two slots of ROWS x (head_dim + 2)
   int32_t* status;
   int n_tokens, n_heads, group, max_q, page, page_shift;

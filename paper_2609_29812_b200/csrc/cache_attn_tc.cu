@@ -168,7 +168,6 @@ __global__ void __launch_bounds__(kThreadsTc, 1) cache_flash_kernel(const __grid
       tc::mbar_init(&ctl.pv_done[t], 1);
     }
     tc::mbar_init(&ctl.open_full, 4);
-    
     for (int s = 0; s < kPlans; ++s) {
       tc::mbar_init(&ctl.plan_full[s], 1);
       tc::mbar_init(&ctl.plan_free[s], kReaders);
