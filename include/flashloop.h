@@ -446,7 +446,7 @@ FL_API int fl_rotate_rows(fl_ctx* ctx, const void* x, int64_t x_stride, const in
 /* A paged K/V cache of n_seqs sequences. A block is `page` consecutive tokens of a sequence; the first floor(n / page) blocks of a
  * sequence of n tokens are held in pages as 8-bit codes with one binary32 scale for each (page, kv head) and side, and the
  * remaining n mod page tokens in the sequence's open block in the storage type (as the recent tail of the packed base is).
- * Block j of sequence b lies in page page_table[b][j]. Value = code * scale.
+ * Block j of sequence b lies in page page_table[b][j]. Value = code * scale, whoever wrote the two; a code is a number.
  *   FL_INT8: two's complement codes in -127 .. 127, scale = max|x| / 127
  *   FL_E4M3: 8-bit floating point (1 sign, 4 exponent, 3 mantissa bits, largest 448), scale = max|x| / 448
  * Head groups: query head h reads kv head h / (n_heads / n_kv_heads). */
@@ -496,8 +496,13 @@ FL_API int fl_cache_read(fl_ctx* ctx, const fl_paged_kv* cache /* host */, const
  * seq_start[b] .. seq_start[b+1]-1 of q (q_stride elements apart, n_heads heads each) are the last n_b tokens of sequence b, whose cache
  * holds kv_len[b] tokens with those included; the row of token p = kv_len[b] - n_b + i sees tokens 0 .. p:
  *   o [n_tokens, n_heads, head_dim] storage type;  lse f32 [n_tokens, n_heads] = log sum exp(sm_scale q.k), or NULL.
- * A row that sees nothing gets o = 0, lse = -inf. What lies beyond a row's last token (stale codes, rows of an open block that were
- * never written, NaN) has no effect on it. max_q: no sequence has more new tokens (a host number that picks the kernels; a
+ * A row that sees nothing gets o = 0, lse = -inf; one that sees a token of a block without a scale that is a number gets NaN for both. What
+ * lies beyond a row's last token (stale codes, rows of an open block that were never written, NaN) has no effect on it but for the last
+ * bits named here: with bf16 storage the products take f16. Codes are exact in it; a query row, and the rows of an open block, are
+ * brought into its range by one power of two for all of them, so that beside the eight bits that they have an element of q and an open key
+ * are held to 2^-39 of the largest there, an open value to 2^-31; and a token's p v is held to 2^-12 of itself or 2^-31 of the largest |v|
+ * of the sequence's kv head, whichever is more, whether the row sees that one or not. Logits, sums and accumulators are binary32, as is
+ * everything with binary32 storage. max_q: no sequence has more new tokens (a host number that picks the kernels; a
  * sequence with more is not computed and sets the status word).
  * workspace: fl_cache_attention_workspace_bytes() bytes of device memory, 256-byte aligned, cleared once before its first use
  * (every call leaves its counters cleared); calls that may overlap in time must not share one.

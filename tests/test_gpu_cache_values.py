@@ -5,7 +5,7 @@ import math
 import pytest
 
 import cache_reference as ref
-from test_gpu_cache import Cache, env, ints, rows, same_bits  # noqa: F401
+from test_gpu_cache import Cache, env, rows  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -140,3 +140,21 @@ def test_every_row_that_sees_a_block_without_a_scale_is_none(env, dtype, new, pa
         if blind:
             want = ref.attention(q[s][:blind].double(), c.held(0, b)[:lens[b] - new + blind], c.held(1, b)[:lens[b] - new + blind], 2, dim ** -0.5)
             ref.assert_attention(o[s][:blind], lse[s][:blind], want, dim, dtype == "bf16", f"sequence {b}")
+
+
+# ------------------------------------------------------------------------------------------------
+# the range that rows beyond a row's own tokens leave it
+# ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,new", KERNELS)
+@pytest.mark.parametrize("page,length", [(64, 640 + 20), (16, 640 + 9), (64, 640), (128, 700)])
+def test_much_larger_rows_that_come_later(env, dtype, new, page, length):
+    """Keys and values 2^20 times larger in the last tokens: rows before them keep the bits that the header promises (an open key 2^-39 of
+    its block's largest, which the bound on the logits holds up to 2^24; p v 2^-31 of the sequence's largest value)."""
+    B, ctx = env
+    c = Cache(B, 1, 720, page=page, dtype=dtype, n_kv=2, dim=128)
+    g = torch.Generator().manual_seed(37)
+    k, v = rows(g, length, 2, 128, c.dt), rows(g, length, 2, 128, c.dt)
+    k[length - 2:] *= 2.0 ** 20
+    v[length - 2:] *= 2.0 ** 20
+    c.append(ctx, [length], k, v, check=False)
+    c.check_attention(ctx, rows(g, new, 4, 128, c.dt), [new], f"{dtype} {new}")
