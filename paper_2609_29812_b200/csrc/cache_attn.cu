@@ -4,9 +4,11 @@
 // take equal runs of the units of all problems, so that one long sequence among short ones, or one sequence alone, fills the chip. The
 // four warps of a CTA take a quarter of a run each, with a running reference and sum of their own per row, and meet in shared memory;
 // a problem that a run's border cuts is put together by the CTA that comes last, in the order of the parts.
-// Bound by HBM where the batch fills the chip, each code read once: 32 sequences of up to 16384 tokens x 16 heads 208 us = 6.1 TB/s (with
-// copies by the lanes in place of the ring of tiles 320, whatever their number on the way); by latency where it does not: one row over 8192
-// tokens 16 us (floor 5), of which the first pages, the join and the launch are 8.
+// Bound by HBM where the batch fills the chip, each code read once: 32 sequences of up to 16384 tokens x 16 heads 208 us = 6.1 TB/s
+// call after call on the same cache, 240 us = 5.3 TB/s on one cache after another (with copies by the lanes in place of the ring of tiles
+// 320, whatever their number on the way); an instruction leaves in 59% of the cycles then. By latency where it does not: one row over
+// 8192 tokens 16 us (18.7 on changing caches; floor 5), of which the first pages, the join and the launch are 8. With 16 rows (254 registers, eight warps an
+// SM) an instruction leaves in 27% of the cycles, and the warps wait for the next one to be fetched more than for anything else.
 #include "cache_attn.cuh"
 
 namespace {
@@ -213,7 +215,8 @@ struct MmaEngine {
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[n][nb][e] *= ks[n] * unit[nb][e & 1];
-    if (t0 + 16 * N > whole) {                       // (uniform: a row's limit, or the warp's last tile, lies in these tiles)
+    if (t0 + 16 * N > whole) {                       // (uniform: a row's limit, or the warp's last tile, lies in these tiles; a row
+                                                     // that pads the tile has limit 0, so with fewer rows than it holds in all of them)
 #pragma unroll
       for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -319,7 +322,7 @@ struct MmaEngine {
       raise(__uint_as_float(__reduce_max_sync(0xffffffffu, w.vs < INFINITY ? __float_as_uint(w.vs) : 0u)));
     };
     fill(ta >> sh);
-    int whole = tb * 16;                                      // tokens that every row sees
+    int whole = tb * 16;                                      // tokens that every row of the tile sees (0 where some are padding)
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -514,9 +517,10 @@ struct MmaEngine {
 // ------------------------------------------------------------------------------------------------------------
 // Binary32 storage: the same work on the FMA pipe. A pair of lanes has a token of the tile for the first product, a lane four (two)
 // dims for the second; Q rows and probabilities stand in shared memory. With one row per kv head the conversions cost as much as the products.
-// Bound by the FMA pipe's instructions (two conversions and a product per code and row, 255 registers, eight warps an SM), the next tile's codes on
-// their way meanwhile: 32 sequences of up to 16384 tokens 1306 us, 2546 with each tile's loads in its own loops; 256 rows x 16 heads on 4096 tokens
-// 819 us = 10 TFLOP/s for 2608, where limits and visibility were looked up for every token.
+// Bound by its instructions at eight warps an SM (255 registers, 64 bytes of spills with heads of 128): one leaves in 53% of the cycles; ALU
+// (conversions) 35%, FMA 29%, LSU 24% of their rates. The next tile's codes are on their way meanwhile: 32 sequences of up to 16384 tokens
+// 1299 us, 2546 with each tile's loads in its own loops; 256 rows x 16 heads on 4096 tokens 817 us = 10 TFLOP/s, 2608 where limits and
+// visibility were looked up for every token.
 // ------------------------------------------------------------------------------------------------------------
 template <int DH, int CODE>
 struct SimtEngine {

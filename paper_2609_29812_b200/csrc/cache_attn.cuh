@@ -7,7 +7,14 @@ namespace fl_ca {
 
 // Which kernel takes a sequence (each looks for itself; lengths stand on the device): the one for few rows up to 16 rows (new tokens x
 // group), and up to 128 where all there is to do is little, for it starts sooner; over long caches the other one multiplies faster.
-// One sequence, 16 kv heads, 64 new tokens, few / many: after 448 tokens 27 / 31 us, after 4032 38 / 43 us.
+// One sequence, 16 kv heads, few / many, us:
+//   tokens            512        1024        2048        4096        8192       16384
+//    32 rows      26 / 32     27 / 32     28 / 37     32 / 41     39 / 54     52 / 76
+//    64 rows      27 / 32     28 / 33     31 / 37     38 / 41     50 / 55     78 / 77
+//   128 rows      28 / 33     33 / 33     39 / 37     52 / 41     78 / 52    128 / 73
+// The border lies at 64 rows x 4096 tokens, 128 x 2048: where 128 rows cross; fewer rows would cross later, for the tiles of 16 that read the
+// same codes again are what costs the first kernel. All sequences count, those without new tokens too: the number of them is all that
+// the host knows.
 constexpr int kFewRows = 16;
 constexpr int64_t kLittle = 1 << 22;   // rows x tokens x kv heads x sequences
 enum { kEvery = 0, kFew = 1, kMany = 2 };
@@ -210,7 +217,8 @@ constexpr float kMove = 8.f;       // log2: how far a logit may pass the referen
 __device__ __forceinline__ float part_weight(float m, float top) { return m == -INFINITY ? 0.f : tc::ex2(m - top); }
 
 // Two codes (bytes SEL and SEL + 1 of a word) as a pair of f16, exactly.
-//   int8: the byte plus 128 in the low bits of 1024 is the number 1152 + code.
+//   int8: the byte plus 128 in the low bits of 1024 is the number 1152 + code (the magic-number conversion: an integer set into the
+//   mantissa of a number whose unit is its last place).
 //   e4m3: one conversion (as fast as a byte permutation).
 template <int CODE, int SEL>
 __device__ __forceinline__ uint32_t code_pair(uint32_t w) {

@@ -8,10 +8,12 @@
 // two tiles use them up, and the scales never touch the operands: a block's scale of K goes into the factor of its
 // columns' logits, its scale of V into the exponent of their probabilities, P' = 2^(s - ref + log2(2^7 vs / vref)), vref the largest scale
 // so far, and the row's sum takes P' back in 32 bits.
-// Bound by neither products nor exponentials but by instructions: a chunk takes 6000 cycles where its products take 2000, the warps of the
-// softmax and those of the codes are at work nearly all of them, and get an instruction off in eight to ten cycles, for the code of
-// four roles is more than the instruction caches serve. 2048 rows x 16 heads on 32768 tokens, int8: 720 us = 740 TFLOP/s; with an eighth of
-// the products, without the exponentials and with a sixteenth of the codes turned it takes 770, 630 and 780.
+// Bound by neither products nor exponentials alone: a chunk takes 6000 cycles where its products take 2000. With clocks read around the waits
+// (8200 cycles a chunk) the warps of the codes work 4900 to 5600 of them, the softmax of the two tiles waits 800 and 2000, and Q K^T waits
+// 3250 for the other tile to take its S; a warp gets an instruction off in eight to ten cycles, a fifth of them for want of the next one:
+// the code of four roles is more than the instruction caches serve, and where it comes to lie moves the time by 3% either way. 2048 rows x
+// 16 heads on 32768 tokens: int8 730, e4m3 729, pages of 16 806 us (730 = 727 TFLOP/s; 748 on one cache after another). At 720, with an eighth of
+// the products, without the exponentials and with a sixteenth of the codes turned it took 770, 630 and 780.
 #include "cache_attn.cuh"
 
 namespace {
@@ -22,8 +24,8 @@ using namespace fl_tc;
 constexpr int kRows = 256, kNC_ = 128, kSlots = 4;
 constexpr int kWarpsTc = 16, kThreadsTc = kWarpsTc * 32;
 // warps 0-3, 4-7: softmax of a tile; 8: QK^T; 9: PV; 10: the plan; 11: pages and scales; 12-15: codes to operands. Registers of the four
-// warpgroups: 2 x 192 + 64 + 64 of 512. int8 / e4m3 / pages of 16: 716 / 748 / 797 us so, 748 / 737 / 827 with 208 + 48 + 48,
-// 702 / 767 / 779 with 192 + 56 + 72, 771 / 765 / 798 with 184 + 64 + 80.
+// warpgroups: 2 x 192 + 64 + 64 of 512. int8 / e4m3 / pages of 16 when they were chosen: 716 / 748 / 797 us so, 748 / 737 / 827 with 208 + 48
+// + 48, 702 / 767 / 779 with 192 + 56 + 72, 771 / 765 / 798 with 184 + 64 + 80.
 constexpr int kQkWarp = 8, kPvWarp = 9, kPlanWarp = 10, kScaleWarp = 11, kCodeWarp = 12;
 constexpr int kReaders = 15;           // warps that read the plan: softmax, issuers, scales, codes
 constexpr int kRegsSoftmax = 192, kRegsIssue = 64, kRegsCodes = 64;

@@ -50,9 +50,11 @@ template <typename T> __device__ __forceinline__ uint32_t top_bits(uint32_t m) {
 // the input, rotated with cosines and sines that serve all of the CTA's heads), their largest magnitude taken over the CTA, coded
 // and written: one pass over the data. The block that stays open is written by the sequence's first CTA, after it has read the rows that
 // the open block held, so no two CTAs touch an open block.
-// Bound by HBM, 2 (4) bytes an element in and 1 out: 32768 tokens of 16 heads 86 us = 4.9 TB/s with the rotation, 76 without:
-// the pairs' products and the codes' conversions are what is left. It lives on loads on their way: with numbers in place of the stored
-// pieces and room for four items in every instance one CTA fitted an SM (164 registers).
+// 2 (4) bytes an element in and 1 out: 32768 tokens of 16 heads 86 us = 4.9 TB/s with the rotation, 76 without. Between HBM (54% of its
+// nominal rate) and instructions (one leaves in 68% of the cycles; ALU 54%, conversions 37% of their rates). It lives on loads on their way: with
+// numbers in place of the stored pieces and room for four items in every instance one CTA fitted an SM (164 registers). binary32: 177 us
+// (floor 105), one CTA of eight warps an SM; 137 with pages of 128, whose CTAs have sixteen. Rotations that are no multiple of 16 elements, and rows
+// off 16-byte boundaries, go element by element and head by head: 195 us, binary32 446.
 template <typename T, int CODE, int MODE>
 __device__ __forceinline__ void append_block(const AppendArgs& a, const Block& k, int side, int head0, int page, int head_dim, int page_id, int slot) {
   constexpr int ITEMS = 2;
@@ -313,7 +315,7 @@ int append(fl_ctx* ctx, AppendArgs& a, const fl_paged_kv* c, int mode, bool vec,
 // ------------------------------------------------------------------------------------------------------------
 // Rows read back. A CTA has 16 consecutive rows; a thread 16 elements of one (row, head): 8 threads (4 with heads of 64) per
 // 128-byte row of codes, four consecutive tokens per warp, so that a warp reads 512 bytes of a page in one go and writes four
-// whole rows of a head. Bound by HBM, 1 byte in, 2 (4) out: 32768 tokens of 16 heads 69 us = 5.9 TB/s.
+// whole rows of a head. Bound by HBM, 1 byte in, 2 (4) out: 32768 tokens of 16 heads 68 us = 5.9 TB/s (a warp waits 12 cycles of 23 for its loads).
 // ------------------------------------------------------------------------------------------------------------
 constexpr int kReadRows = 16;
 
