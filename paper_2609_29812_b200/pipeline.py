@@ -412,7 +412,8 @@ class RotaryTable:
 class PagedCache:
     """A paged 8-bit K/V cache of one layer and the calls on it: pages are handed out on the host as sequences grow, everything else stays
     on the device.  `code`: B.FL_INT8 or B.FL_E4M3.  On more than one stream calls are ordered by the program, as with any tensors: append
-    and release write what attend and read look at.  Those two may run beside one another; each stream has a workspace of its own."""
+    and release write what attend and read look at.  Those two may run beside one another; each stream has a workspace of its own.
+    In a captured graph they go by the lengths that were there at the capture, until the next append lets go of them."""
 
     def __init__(self, ctx, n_seqs: int, n_kv_heads: int, head_dim: int, max_tokens: int, n_pages: Optional[int] = None, page: int = 64,
                  dtype=torch.bfloat16, code=B.FL_INT8, device="cuda:0"):

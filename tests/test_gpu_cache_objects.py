@@ -64,3 +64,33 @@ def test_the_example_s_second_loop_starts_from_the_cache():
         assert_attn_close(to_np(d["o2"]), want["O"], f"example, token {i}")
         np.testing.assert_allclose(to_np(d["lse2"]), want["lse"], rtol=0, atol=5e-3)
         assert np.linalg.norm(want["O"] - to_np(d["o1"])) > 5 * 1e-2 * np.linalg.norm(want["O"])    # (what loop 2 does is well above the bound)
+
+
+def test_a_captured_attend_has_a_workspace_of_its_own():
+    from paper_2609_29812_b200 import binding as B, pipeline as P
+    with B.Context(0) as ctx:
+        c = P.PagedCache(ctx, 1, 2, 64, 3000)
+        g = torch.Generator(device="cuda").manual_seed(1)
+        x = torch.randn(3000, 2, 64, generator=g, device="cuda").to(torch.bfloat16)
+        c.append(x[:2999], x[:2999], [2999])
+        q = x[:1].clone()
+        one = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+        want = c.attend(q, [1], 0.125, one)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            o, lse = c.attend(q, [1], 0.125, one)
+        again = c.attend(q, [1], 0.125, one)                    # what the capture allocated is not in the way of later calls
+        assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1])
+        for _ in range(3):
+            o.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+        q.copy_(x[7:8])
+        graph.replay()
+        other = c.attend(q, [1], 0.125, one)
+        assert torch.equal(o, other[0]) and not torch.equal(o, want[0])
+        c.check_status()
+        c.append(x[2999:], x[2999:], [1])                       # (lets go of the lengths that the graph reads)
+        torch.cuda.synchronize()
+        del graph
